@@ -254,7 +254,9 @@ class DQTDecoder(torch.nn.Module):
         self.register_buffer("inv_freq", 1.0 / (cfg.rope_theta ** (torch.arange(0, hd, 2, device=device,
                                                                                   dtype=torch.float32) / hd)),
                              persistent=False)
-        self._rect_plan = (None, None)  # (batch, length) of the last rectangular batch that needed one
+        # (batch, length, device): the plan of a rectangular batch with shared heads.  Kept as long as
+        # the model: captured graphs, and calls queued on other streams, read its table by address.
+        self._rect_plans = {}
 
     def bitlinear_layers(self):
         return [m for m in self.modules() if isinstance(m, DQTBitLinear)]
@@ -295,6 +297,12 @@ class DQTDecoder(torch.nn.Module):
         """The bf16 parameters an ordinary optimiser trains (not the BitLinear codes)."""
         return [p for n, p in self.named_parameters() if not n.endswith("_anchor")]
 
+    def _rect_plan(self, batch, length, device):
+        plan = self._rect_plans.get((batch, length, device))
+        if plan is None:  # (of two threads that make it at once both take the first's)
+            plan = self._rect_plans.setdefault((batch, length, device), dqt.attn_plan([length] * batch, device))
+        return plan
+
     def _logits(self, ids, plan):
         """Logits [B, S, V] of ids [B, S], or of the documents of a plan as [1, tokens, V]."""
         if plan is not None:
@@ -306,9 +314,7 @@ class DQTDecoder(torch.nn.Module):
             B, S = ids.shape
             t = torch.arange(S, device=ids.device, dtype=torch.float32)
             if self.cfg.kv_heads != self.cfg.heads:  # shared heads: the library's attention
-                if self._rect_plan[0] != (B, S, ids.device):
-                    self._rect_plan = ((B, S, ids.device), dqt.attn_plan([S] * B, ids.device))
-                plan = self._rect_plan[1]
+                plan = self._rect_plan(B, S, ids.device)
         x = F.embedding(ids, self.embed)
         ang = torch.outer(t, self.inv_freq)
         cos_sin = torch.stack((torch.cos(ang), torch.sin(ang)), dim=-1)  # [S, D/2, 2]
