@@ -1144,13 +1144,24 @@ class AttnPlan:
     def positions(self):
         """int64 [tokens]: each token's position in its document."""
         if self._positions is None:
+            _no_capture("AttnPlan.positions", self.table.device)
             self._positions = torch.cat([torch.arange(n) for n in self.lengths]).to(self.table.device)
         return self._positions
 
 
+def _no_capture(what, device):
+    """What copies from the host's pageable memory cannot be part of a CUDA graph."""
+    if device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("%s copies from host memory and cannot run while a CUDA graph is captured: "
+                           "call it once before" % what)
+
+
 def attn_plan(lengths, device="cuda"):
     """AttnPlan of documents of these lengths (host integers, 0 allowed), packed in order.
-    The table is copied to the device on the current stream."""
+    The table is copied to the device on the current stream, and is there on return; not during the
+    capture of a CUDA graph.  Calls read it by address: keep the plan as long as captured graphs
+    that use it are replayed."""
+    _no_capture("attn_plan", torch.device(device))
     lengths = tuple(int(n) for n in lengths)
     if not lengths or min(lengths) < 0 or sum(lengths) < 1:
         raise ValueError("lengths must hold a positive number of tokens and no negative length")
