@@ -1203,6 +1203,9 @@ def _attn_layout(q, k, v, plan):
                          % (T, D, tuple(k.shape), tuple(v.shape)))
     if KV == 0 or H == 0 or H % KV:
         raise ValueError("q has %d heads, not a multiple of k's and v's %d" % (H, KV))
+    if not (plan.table.device == q.device == k.device == v.device):
+        raise ValueError("the plan, q, k and v must be on one device, got %s, %s, %s and %s"
+                         % (plan.table.device, q.device, k.device, v.device))
     qs, ks, vs = q.stride(), k.stride(), v.stride()
     return dqt_attn_layout_t(T, plan.tiles, plan.tiles256, plan.longest, H, KV, D, qs[0], qs[1], ks[0], ks[1], vs[0],
                              vs[1])
