@@ -186,9 +186,10 @@ __device__ __forceinline__ dqt_attn_tile_t tile_of(const dqt_attn_tile_t* tiles,
   return {v.x, v.y, v.z, v.w};
 }
 
-// A tile that lies in the tensors, and its slot in the workspace; others are left out.
+// A tile that lies in the tensors, and its slot in the workspace; others are left out.  (Rows start
+// at multiples of 128: the slots of a document's other rows are counted from that.)
 __device__ __forceinline__ bool tile_ok(const dqt_attn_tile_t& t, const dqt_attn_layout_t& L) {
-  return t.start >= 0 && t.row >= 0 && t.row < t.len && t.start + static_cast<int64_t>(t.len) <= L.tokens &&
+  return t.start >= 0 && t.row >= 0 && (t.row & 127) == 0 && t.row < t.len && t.start + static_cast<int64_t>(t.len) <= L.tokens &&
          t.slot >= t.row >> 7 && t.slot + static_cast<int64_t>((t.len - t.row + 127) >> 7) <= L.tiles;
 }
 
