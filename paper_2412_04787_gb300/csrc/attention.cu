@@ -768,7 +768,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 //
 // lse and delta belong to lanes in the dQ kernel, which takes delta from do and o and writes both for the
 // other kernel, whose columns they belong to: as three bf16 each (24 bits), which a product of 16 columns with
-// ones adds to X and Y.  Read from shared memory instead, 8 bytes for each of a thread's columns, they were
+// ones adds to X and Y.  Each has a row of its own, so that a delta that is not finite meets no zero in X
+// (dv does not depend on it).  Read from shared memory instead, 8 bytes for each of a thread's columns, they were
 // as much traffic there as the operands (8 x 2048, 32 heads: 286 us, and 254 so).
 //
 // W is 128 for dim 64: with steps of 64 rows the warps' waits alone took 635 clk a step of
@@ -793,10 +794,11 @@ struct BwdSmem {
   static constexpr int RBUF = D == 64 ? 2 : 1;          // buffers of them
   static constexpr int RING = 4;                        // stages of two blocks
   static constexpr int RING_OFF = RBUF * NR * RES;
-  // KV: the stages' lse and delta, ones for X and for Y, zeros; dQ: lse and delta of two items
+  // KV: the stages' lse and delta, ones, zeros; dQ: lse and delta of two items
   static constexpr int STAT_OFF = RING_OFF + RING * 2 * BLK;
-  static constexpr int ONES_OFF = STAT_OFF + RING * W * 16;
-  static constexpr int ZERO_OFF = ONES_OFF + 2 * 2048;
+  static constexpr int STAT = W * 16;  // lse, or delta, of a stage
+  static constexpr int ONES_OFF = STAT_OFF + RING * 2 * STAT;
+  static constexpr int ZERO_OFF = ONES_OFF + 2048;
   static constexpr int OUT_OFF = KV ? ZERO_OFF + 2048 : STAT_OFF + 2 * 2 * 512;
   static constexpr int INFO_OFF = OUT_OFF + 4 * 2048;  // what the math warps know of two items
   static constexpr int BAR_OFF = INFO_OFF + 2 * 32;
@@ -812,7 +814,7 @@ struct BwdSmem {
   static constexpr int NA = (512 - NXY * W) / ACC < 2 ? 1 : 2;
   static_assert(NX >= 2 && NY >= 1 && RING >= NX, "tensor memory");
   static_assert((2 * RING + 2 * RBUF + 2 * NX + 2 * NY + 2 * NA + 2 + 3) * 8 + 4 <= 384, "barriers");
-  static constexpr uint32_t STAGE_TX = 2 * BLK + (KV ? 16 * W : 0);
+  static constexpr uint32_t STAGE_TX = 2 * BLK + (KV ? 2 * STAT : 0);
 };
 
 struct BwdParams {
@@ -826,7 +828,7 @@ struct BwdParams {
   float scale, inv_scale, scale_log2;
   const float* lse;      // dQ
   const uint16_t* o;     // dQ
-  uint4* stat;           // [heads, tiles * 128]: dQ writes, KV reads
+  uint4* stat;           // [2, heads, tiles * 128], lse and delta: dQ writes, KV reads
   uint16_t* out0;  // dq, or dv
   uint16_t* out1;  // dk
   uint64_t wait_ns;
@@ -962,8 +964,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (KV && threadIdx.x < 128) {
     uint4* at = reinterpret_cast<uint4*>(smem + S::ONES_OFF) + threadIdx.x;
     at[0] = make_uint4(0x3F803F80u, 0x00003F80u, 0, 0);
-    at[128] = make_uint4(0, 0x3F800000u, 0x3F803F80u, 0);
-    at[256] = make_uint4(0, 0, 0, 0);
+    at[128] = make_uint4(0, 0, 0, 0);
     fence_async_shared();
   }
   if (warp == 9) tmem_alloc(slot, 512);
@@ -1048,8 +1049,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t a[3], e[3];
         pieces(-lse * p.inv_scale, a);
         pieces(nd, e);
-        p.stat[static_cast<int64_t>(x.head) * p.L.tiles * 128 + static_cast<int64_t>(x.t.slot) * 128 + row] =
-            make_uint4(a[0] | a[1] << 16, a[2] | e[0] << 16, e[1] | e[2] << 16, 0);
+        const int64_t of_row = (static_cast<int64_t>(x.head) * p.L.tiles + x.t.slot) * 128 + row;
+        p.stat[of_row] = make_uint4(a[0] | a[1] << 16, a[2], 0, 0);
+        p.stat[p.L.heads * p.L.tiles * 128 + of_row] = make_uint4(e[0] | e[1] << 16, e[2], 0, 0);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&info_full[info.i]);
@@ -1141,7 +1143,9 @@ __global__ void __launch_bounds__(kThreads, 1)
               // the block's rows in the slots of its document
               const int64_t at = static_cast<int64_t>(h) * p.L.tiles * 128 +
                                  (static_cast<int64_t>(x.t.slot) - x.t.row / 128) * 128 + S::W * b;
-              bulk_load(smem + S::STAT_OFF + s * S::W * 16, p.stat + at, S::W * 16, &full[s]);
+              for (int m = 0; m < 2; ++m)
+                bulk_load(smem + S::STAT_OFF + (2 * s + m) * S::STAT, p.stat + m * p.L.heads * p.L.tiles * 128 + at,
+                          S::STAT, &full[s]);
             }
             if (++b == x.b1) {
               b = x.b0;
@@ -1164,7 +1168,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t base = smem_u32(smem) + m * S::RES, ring = smem_u32(smem) + S::RING_OFF + m * S::BLK;
       const uint32_t d0 = tmem + (m ? S::Y_COL : 0);
       uint64_t* done_bar = m ? y_full : x_full;
-      const uint64_t ones = sdesc_pieces(smem_u32(smem) + S::ONES_OFF + m * 2048, smem_u32(smem) + S::ZERO_OFF);
+      const uint64_t ones = sdesc_pieces(smem_u32(smem) + S::ONES_OFF, smem_u32(smem) + S::ZERO_OFF);
       Waits wait{p.wait_ns};
       Ring<S::RING> stage, before;  // the step's stage, and that of the step whose columns X takes
       Ring<S::RBUF> res;
@@ -1195,7 +1199,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         k > 0 ? 1u : 0u);
             if (KV)
               umma_bf16(d, ones,
-                        sdesc_pieces(smem_u32(smem) + S::STAT_OFF + stage.i * S::W * 16,
+                        sdesc_pieces(smem_u32(smem) + S::STAT_OFF + (2 * stage.i + m) * S::STAT,
                                      smem_u32(smem) + S::ZERO_OFF),
                         kIdescXY, 1u);
             umma_commit(&done_bar[col]);
@@ -1476,7 +1480,7 @@ int bwd(const uint16_t* dout, const uint16_t* q, const uint16_t* k, const uint16
   p.out1 = dk;
   p.split = Div(bwd_split(L));
   p.per = Div(L.kv_heads * p.split.d);
-  p.part = ws + L.heads * L.tiles * 512;
+  p.part = ws + L.heads * L.tiles * 1024;
   p.items *= static_cast<int>(p.split.d);
   const int rc2 = launch_dep(kkv, dim3(ctas(p.items)), kThreads, BwdSmem<D, true>::BYTES, stream, rk, rv, sq,
                              sdo, p);
@@ -1497,7 +1501,7 @@ int launch_attn_fwd(const uint16_t* q, const uint16_t* k, const uint16_t* v, con
 size_t attn_bwd_ws(const dqt_attn_layout_t& L) {
   const int split = bwd_split(L);
   const size_t rows = static_cast<size_t>(L.tiles) * 128;
-  return (rows * L.heads * 4 + (split > 1 ? rows * L.kv_heads * L.dim * 2 * split : 0)) * sizeof(float);
+  return (rows * L.heads * 8 + (split > 1 ? rows * L.kv_heads * L.dim * 2 * split : 0)) * sizeof(float);
 }
 
 int launch_attn_bwd(const uint16_t* dout, const uint16_t* q, const uint16_t* k, const uint16_t* v,
