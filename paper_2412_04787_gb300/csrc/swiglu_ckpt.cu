@@ -33,13 +33,33 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// 1 / (1 + exp(-x)) to 2^-21 relative (exactly rounded functions took the forward from 110 to
-// 161 us at 16384 x 5632: it was bound by their instructions)
+__device__ __forceinline__ uint16_t bf16(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+
+// 1 / (1 + exp(-x)) for |x| < 80, to 2^-17 relative (x log2 e of 64 and more is off by 2^-17 in fp32),
+// beside the 2^-9 of the results' rounding.  (Exactly rounded functions took the forward from 110 to
+// 161 us at 16384 x 5632: it was bound by their instructions.)
 __device__ __forceinline__ f32x2 sigmoid2(f32x2 x) {
   const f32x2 e = mul2(x, pack2(-1.4426950408889634f, -1.4426950408889634f));
   const float2 d = unpack2(add2(exp2_approx2(e), pack2(1.0f, 1.0f)));
   return pack2(rcp_approx(d.x), rcp_approx(d.y));
 }
+
+// Blocks with a g of 80 and more take these: for large g 1 - s loses what g multiplies, and for g < -87
+// s leaves the normal numbers, but s u need not.  With e = exp(-|g| / 2), r = 1 / (1 + e^2):
+// s = r, 1 - s = e^2 r above 0 and the other way round below, and e is multiplied in twice.
+// One value at a time from memory, so that the other blocks' registers stay as few.
+struct Far {
+  float x, e, r;
+  __device__ __forceinline__ explicit Far(float x_) : x(x_), e(expf(-0.5f * fabsf(x_))), r(1.0f / (1.0f + e * e)) {}
+  // s x f
+  __device__ __forceinline__ float silu(float f) const { return x < 0.0f ? x * e * r * f * e : x * r * f; }
+  // s (1 + x (1 - s)) f d
+  __device__ __forceinline__ float slope(float f, float d) const {
+    return x < 0.0f ? (1.0f + x * r) * e * r * f * d * e : (1.0f + x * (e * e * r)) * r * f * d;
+  }
+};
+constexpr uint32_t kFarBits = 0x42A0u;       // 80 as bf16
+constexpr float kFarScale = 80.0f / 127.0f;  // and the scale of its block
 
 // Blocks of 128 columns per row, and n / nb for n < 2^31 as a product (magic = ceil(2^(32 + s) / nb)
 // with 2^s < nb <= 2^(s + 1), so magic nb - 2^(32 + s) < 2^(s + 1) and the quotient is exact).
@@ -153,6 +173,12 @@ __global__ void __launch_bounds__(kThreads)
     if (!p[k].in) continue;
     __stcs(reinterpret_cast<uint2*>(codes + row * 2 * c.F + p[k].col), cg);
     __stcs(reinterpret_cast<uint2*>(codes + (row * 2 + 1) * c.F + p[k].col), cu);
+    if (ag >= kFarBits) {
+      const int64_t at = row * c.F + p[k].col;
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j) h[at + j] = bf16(Far(bf16_lo(g[at + j])).silu(bf16_lo(u[at + j])));
+      continue;
+    }
     const uint32_t gw[4] = {gv[k].x, gv[k].y, gv[k].z, gv[k].w}, uw[4] = {uv[k].x, uv[k].y, uv[k].z, uv[k].w};
     uint32_t o[4];
 #pragma unroll
@@ -195,6 +221,18 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
   for (int k = 0; k < kItems; ++k) {
     if (!p[k].in) continue;
+    const int64_t at = static_cast<int64_t>(p[k].row) * c.F + p[k].col;
+    if (!(sg[k] < kFarScale)) {
+      const int8_t* cr = codes + at + p[k].row * c.F;
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j) {
+        const Far x(cr[j] * sg[k]);
+        const float d = bf16_lo(dh[at + j]);
+        dg[at + j] = bf16(x.slope(cr[c.F + j] * su[k], d));
+        du[at + j] = bf16(x.silu(d));
+      }
+      continue;
+    }
     const uint32_t dw[4] = {dv[k].x, dv[k].y, dv[k].z, dv[k].w};
     uint32_t og[4], ou[4];
 #pragma unroll
@@ -208,7 +246,6 @@ __global__ void __launch_bounds__(kThreads)
       og[j] = pack_bf16x2(rg.x, rg.y);
       ou[j] = pack_bf16x2(ru.x, ru.y);
     }
-    const int64_t at = static_cast<int64_t>(p[k].row) * c.F + p[k].col;
     __stcs(reinterpret_cast<uint4*>(dg + at), make_uint4(og[0], og[1], og[2], og[3]));
     __stcs(reinterpret_cast<uint4*>(du + at), make_uint4(ou[0], ou[1], ou[2], ou[3]));
   }
