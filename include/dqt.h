@@ -710,7 +710,8 @@ int dqt_token_logprob_bf16(const dqt_bf16* logits, int64_t ld, const int64_t* ta
 /* The logits' gradient for upstream dlogp and dentropy (fp32 [M]):
  *   dlogits_v = dlogp ([v = t] - p_v) - dentropy p_v (log p_v + entropy)
  * in fp32, rounded once to bf16; dlogp counts as 0 for a target outside [0, V),
- * and a row of -inf alone gets zeros.  dlogits bf16 [M, V] contiguous, not
+ * and a row of -inf alone gets zeros.  (p is formed from lse; where |lse| is above 1024, and
+ * so too coarse in fp32 for that, from the row's maximum and sum, found again.)  dlogits bf16 [M, V] contiguous, not
  * overlapping logits. */
 int dqt_token_logprob_bwd_bf16(const dqt_bf16* logits, int64_t ld, const int64_t* targets,
                                const float* lse, const float* entropy, const float* dlogp,

@@ -343,16 +343,48 @@ __global__ void __launch_bounds__(NT)
   }
 }
 
-// The gradient of two neighbouring logits
+// The gradient of a logit
 struct Grad {
   float l, c, de, dl;  // lse, dlogp + dentropy * entropy, dentropy, dlogp
-  __device__ __forceinline__ float operator()(float x, bool target) const {
+  __device__ __forceinline__ float operator()(float x, bool target) const { return of(x - l, target); }
+  __device__ __forceinline__ float of(float logp, bool target) const {
     // (held off -inf, so that a logit without probability gets 0; a NaN in c reaches all)
-    const float lp = fmaxf(x - l, kFar);
+    const float lp = fmaxf(logp, kFar);
     const float d = -exp2_approx(lp * kLog2e) * fmaf(de, lp, c);
     return target ? d + dl : d;
   }
 };
+
+// Beyond this |lse|, half a step of which puts 2^-15 into p, a row's lse may say too little about
+// its log S: a row of bf16's lowest value alone has lse = max in fp32, and p = 1 from it.
+constexpr float kLseLimit = 1024.0f;
+
+// Such a row: max and log S found anew, one logit at a time.
+template <int NT>
+__device__ __forceinline__ void far_row(const Row& row, const Grad& g, int64_t t, uint16_t* out) {
+  __shared__ Part parts[NT / 32];
+  Part p = {-INFINITY, 0.0f, 0.0f};
+  auto joined = [&] {
+#pragma unroll 1
+    for (int off = 16; off > 0; off >>= 1)
+      p = join(p, {__shfl_xor_sync(~0u, p.m, off), __shfl_xor_sync(~0u, p.s, off), 0.0f});
+  };
+#pragma unroll 1
+  for (int64_t v = threadIdx.x; v < row.V; v += NT) {
+    const float f = bf16f(row.x[v]);
+    if (f > p.m) p = shifted(p, f);
+    add(p, f);
+  }
+  joined();
+  if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = p;
+  __syncthreads();
+  p = (threadIdx.x & 31) < NT / 32 ? parts[threadIdx.x & 31] : Part{-INFINITY, 0.0f, 0.0f};
+  joined();
+  const float m = __shfl_sync(~0u, p.m, 0), log_s = kLn2 * log2f(__shfl_sync(~0u, p.s, 0));
+#pragma unroll 1
+  for (int64_t v = threadIdx.x; v < row.V; v += NT)
+    out[v] = __bfloat16_as_ushort(__float2bfloat16_rn(g.of((bf16f(row.x[v]) - m) - log_s, v == t)));
+}
 
 // One block per row; 16-byte vectors where the rows of logits and gradient
 // stand alike to a 16-byte boundary (VEC), else single values.  NT threads: 128 up to 8192 logits,
@@ -384,6 +416,10 @@ __global__ void __launch_bounds__(NT)
   const bool none = g.l == -INFINITY;  // a row of -inf alone
   if (none) g = {0.0f, 0.0f, 0.0f, 0.0f};
   uint16_t* out = dx + r * V;
+  if (fabsf(g.l) > kLseLimit) {  // (not a NaN)
+    far_row<NT>(row, g, t, out);
+    return;
+  }
   auto one = [&](int64_t v) {
     out[v] = none ? 0 : __bfloat16_as_ushort(__float2bfloat16_rn(g(bf16f(row.x[v]), v == t)));
   };
