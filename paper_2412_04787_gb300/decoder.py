@@ -32,6 +32,7 @@ plan), ``ckpt8`` keeps the SwiGLU gate's inputs for the backward in 8 bits, and
 
 import torch
 import torch.nn.functional as F
+from torch.autograd.function import once_differentiable
 from torch.nn.attention import SDPBackend, sdpa_kernel
 
 from . import dqt
@@ -137,6 +138,7 @@ class _SwiGLUCkpt(torch.autograd.Function):
         return h.view(g.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh):
         codes, scales = ctx.saved_tensors
         dg, du = dqt.dqt_swiglu_ckpt_bwd_bf16(dh.reshape(-1, dh.shape[-1]).contiguous(), codes, scales)
@@ -154,6 +156,7 @@ class _PackedAttention(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         q, k, v, o, lse = ctx.saved_tensors
         return (*dqt.dqt_attn_bwd_bf16(do.contiguous(), q, k, v, o, lse, ctx.plan), None)
@@ -172,6 +175,7 @@ class _TokenLogprob(torch.autograd.Function):
         return logp, entropy, ids, best
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dlogp, dentropy, _ids, _best):
         logits, targets, lse, entropy = ctx.saved_tensors
         return dqt.dqt_token_logprob_bwd_bf16(logits, targets, lse, entropy, dlogp.contiguous(),
