@@ -26,7 +26,7 @@ one token axis: ``plan = dqt.attn_plan(lengths)``, then ``model(ids, targets,
 plan=plan)`` with ids [tokens].  Attention then runs on this library's kernels,
 document by document, and positions start at 0 in each.  ``kv_heads`` shares k
 and v heads between groups of q heads (on those kernels too, with or without a
-plan), ``ckpt8`` keeps the SwiGLU gate's inputs for the backward in 8 bits, and
+plan; their head sizes are 64 and 128), ``ckpt8`` keeps the SwiGLU gate's inputs for the backward in 8 bits, and
 ``model.token_logprobs`` scores given tokens.
 """
 
@@ -47,6 +47,8 @@ _SDPA_BACKENDS = [SDPBackend.FLASH_ATTENTION, SDPBackend.EFFICIENT_ATTENTION]
 
 __all__ = ["DecoderConfig", "DQTDecoder"]
 
+_HEAD_SIZES = (64, 128)  # of this library's attention
+
 
 class DecoderConfig:
     def __init__(self, layers=12, hidden=768, heads=12, ffn=2048, vocab=32000, bits=1.58,
@@ -55,6 +57,8 @@ class DecoderConfig:
         kv_heads = heads if kv_heads is None else kv_heads
         if kv_heads < 1 or heads % kv_heads:
             raise ValueError("heads (%d) must be a multiple of kv_heads (%d)" % (heads, kv_heads))
+        if kv_heads != heads and hidden // heads not in _HEAD_SIZES:
+            raise ValueError("shared k and v heads need a head size of 64 or 128, got %d" % (hidden // heads))
         self.kv_heads, self.ckpt8 = kv_heads, ckpt8
         self.layers, self.hidden, self.heads, self.ffn, self.vocab = layers, hidden, heads, ffn, vocab
         self.bits, self.lr, self.seed, self.act = bits, lr, seed, act
@@ -310,6 +314,9 @@ class DQTDecoder(torch.nn.Module):
     def _logits(self, ids, plan):
         """Logits [B, S, V] of ids [B, S], or of the documents of a plan as [1, tokens, V]."""
         if plan is not None:
+            if self.cfg.hidden // self.cfg.heads not in _HEAD_SIZES:
+                raise ValueError("a plan needs a head size of 64 or 128, got %d"
+                                 % (self.cfg.hidden // self.cfg.heads))
             if ids.numel() != plan.tokens:
                 raise ValueError("ids must hold the plan's %d tokens, got %s" % (plan.tokens, tuple(ids.shape)))
             ids = ids.reshape(1, -1)
