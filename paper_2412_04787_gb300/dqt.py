@@ -1240,6 +1240,8 @@ def dqt_attn_bwd_bf16(do, q, k, v, o, lse, plan, scale=None, ws=None, stream=Non
     if ws is None:
         ws = torch.empty(max(lib().dqt_attn_bwd_workspace_size(C.byref(L)), 16), dtype=torch.uint8,
                          device=q.device)
+        if stream is not None:  # freed on return, and used there until the call is done
+            ws.record_stream(stream)
     _need(ws, "ws", torch.uint8)
     _check(lib().dqt_attn_bwd_bf16(_ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), C.byref(L),
                                    _ptr(plan.table), L.dim ** -0.5 if scale is None else float(scale),
