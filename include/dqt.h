@@ -644,7 +644,10 @@ int dqt_rmsnorm_bwd_bf16(const dqt_bf16* x, const dqt_bf16* w, const float* rstd
  *   o_i = sum_{j <= i} exp(s_ij - lse_i) v_j
  * q head h reads k and v head h / (heads / kv_heads).  A document's values
  * reach no other document's outputs, whatever they are (NaN and infinities
- * included). */
+ * included).  Within a document the places that a row does not see count with a
+ * probability of 0, and 0 times a value that is not finite is NaN: such a value
+ * reaches, besides the rows that see it, those before it in its 128 rows (counted
+ * from the document's first), and in the backward those after. */
 
 /* 128 (or 256) rows of a document: its first token, its length, the tile's
  * first row in it, and how many tiles of 128 rows stand before it in the packing. */
@@ -659,7 +662,8 @@ typedef struct {
  * 128-row tiles by falling number of keys that they see, the same by falling
  * number of rows that see them, then the 256-row tiles by keys seen.  The
  * caller keeps it in device memory, 16-byte aligned, for every call on this
- * packing. */
+ * packing (captured CUDA graphs read it there).  Entries that do not lie in the
+ * tensors, or whose row is no multiple of 128, are left out. */
 int dqt_attn_plan(const int64_t* lengths, int64_t docs, dqt_attn_tile_t* tiles, int64_t cap,
                   int64_t counts[3]);
 

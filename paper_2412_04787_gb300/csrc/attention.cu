@@ -13,6 +13,10 @@
 // tensor cores take no wider operands at this rate: p (its sum l is taken before), and ds.  So o,
 // dv, dq and dk carry a rounding of each term next to that of the result: 0.0025 relative
 // rms for dq and dk, where rounding the result alone gives 0.0017.
+//
+// Masked places: what a row does not see of its own tile of 128 is multiplied by a p or ds of 0, so a
+// value there that is not finite makes the row's sums NaN, as a matrix product with the zeros written out
+// does.  Rows of other documents, and of tiles that a row does not see, reach it in no way.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -194,9 +198,9 @@ __device__ __forceinline__ bool tile_ok(const dqt_attn_tile_t& t, const dqt_attn
 }
 
 // ---------------------------------------------------------------------------
-// Forward on the tensor cores: one persistent CTA per SM, two tiles of 128
-// queries in flight that read the same keys and values, so that one tile's
-// softmax runs beside the other's matrix products.
+// Forward on the tensor cores: a CTA has an SM to itself and goes from one pair of tiles to the
+// next; two tiles of 128 queries in flight that read the same keys and values, so that one
+// tile's softmax runs beside the other's matrix products.
 //
 //   warps 0-3, 4-7  softmax of tile 0 and tile 1: a thread has a query
 //   warp 8          the items, copies (TMA): queries, and a ring of key and value tiles
@@ -220,7 +224,7 @@ __device__ __forceinline__ bool tile_ok(const dqt_attn_tile_t& t, const dqt_attn
 // next that has not started (cluster launch control), so that few uneven pairs fill the SMs: 6063 tokens in 4
 // documents, 16 heads over 2 of 128, 59 us, and 68 with the pairs dealt out in advance.
 //
-// A document of 16384, 32 q heads over 8 of 64: 865 us, 1.27 PFLOP/s, 66 % of the rate of a large matrix
+// A document of 16384, 32 q heads over 8 of 64: 869 us, 1.27 PFLOP/s, 66 % of the rate of a large matrix
 // product.  A pair of blocks takes 1960 clk, in which the exponentials take 1024 of the SM's (32 a clk)
 // and the products 1024: a warp's own chain bounds it (a wait of 150 to 400 clk, the maximum 450, exponentials
 // and sums 950), two warps to a scheduler.  Measured and left: turns for the two warps' exponentials 897 us, a P
@@ -770,17 +774,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 // other kernel, whose columns they belong to: as three bf16 each (24 bits), which a product of 16 columns with
 // ones adds to X and Y.  Each has a row of its own, so that a delta that is not finite meets no zero in X
 // (dv does not depend on it).  Read from shared memory instead, 8 bytes for each of a thread's columns, they were
-// as much traffic there as the operands (8 x 2048, 32 heads: 286 us, and 254 so).
+// as much traffic there as the operands (dk and dv of 8 x 2048, 32 heads, in a form before this one: 286 us, and
+// 254 so).
 //
 // W is 128 for dim 64: with steps of 64 rows the warps' waits alone took 635 clk a step of
 // 980.  For dim 128 shared and tensor memory hold 64.
 //
-// 8 x 2048, 32 heads of 64: dq 194 us, dk and dv 215.  A step of dk and dv (128 x 128) takes 1530 clk, and its
+// 8 x 2048, 32 heads of 64: dq 195 us, dk and dv 222 (215 with lse and delta in one row, of which the stamps
+// that follow are).  A step of dk and dv (128 x 128) takes 1530 clk, and its
 // products keep the tensor cores for 1410 of them (1150 if nothing else used shared memory, which their operands
 // take at the full 128 bytes a clk); one of dq 1400, 1100 of them products.  Dim 128 (6063 tokens, 16 heads
-// over 2): 72 and 104 us, a step of 64 columns 1130 and 1600 clk, products 1020 and 1380 (64 columns take 48 clk
+// over 2): 73 and 109 us, a step of 64 columns 1130 and 1600 clk, products 1020 and 1380 (64 columns take 48 clk
 // for 16 of dim, 128 take 64).  Measured and left: X and Y freed once read and p and ds in columns of their
-// own (dk and dv 250 us), Y in a half for each group (270), four groups for p and ds, resident tiles in
+// own (dk and dv 250 us, beside 214), Y in a half for each group (269, beside 254), four groups for p and ds, resident tiles in
 // tensor memory, heads in sets that fit the L2 (2 % of this case, and 3 % lost to uneven ends of others).
 // ---------------------------------------------------------------------------
 template <int D, bool KV>
