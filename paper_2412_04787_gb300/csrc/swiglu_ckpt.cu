@@ -10,7 +10,7 @@
 // instructions.  Half a warp has the 128 columns that share a scale, a 16-byte
 // vector of g and of u per lane, so that the maximum is four shuffles; a half-warp
 // takes kItems blocks at once to keep that many loads in flight.  16384 x 5632: 117 us, 6.4 TB/s (94 %
-// of a copy's), and backward 102 us, 7.3 TB/s; 3001 x 2744: 14 and 10.6 us.
+// of a copy's), and backward 102 us, 7.3 TB/s; 3001 x 2744: 14 and 10.9 us.
 //
 // The checkpoint is the one rounding of g and u that the backward sees: half a scale, 1 / 254 of
 // the block's largest.  h, dg and du are rounded to bf16 as g and u are; all between is fp32.

@@ -9,9 +9,9 @@
 //
 // Both are bound by memory: one pass over the logits forward (2 bytes a
 // logit), one read and one write backward (4 bytes).  All sums are fp32; dx is rounded to bf16 as its
-// logits are.  16384 x 32000: 170 us, 6.2 TB/s (91 % of a copy's), and with eight alternatives 204 us, whose
+// logits are.  16384 x 32000: 155 us, 6.7 TB/s (99 % of a copy's), and with eight alternatives 203 us, whose
 // search is a chain of some 3 us at the end of a block; 4099 x 50257: 70 us, 5.9 TB/s, and backward
-// 119 us, 6.9 TB/s.  5 rows of 32000, five alternatives: 7 us, a launch and that chain.
+// 119 us, 6.9 TB/s (caches clean; after a write of all of the L2 each takes some 15 us more).  5 rows of 32000, five alternatives: 7 us, a launch and that chain.
 #include <cuda_bf16.h>
 
 #include "dqt_internal.h"

@@ -7,9 +7,9 @@ rounding (Sec. 3.2, Eq. 5).  Here q, k, v, o, gate, up and down are
 the FP8-environment forward of Sec. 4.3); the token
 embedding, the RMSNorm gains and the output head stay in bf16 and are trained
 by an ordinary optimiser (which weights the paper keeps in high precision is
-not stated; this is the BitNet convention).  Causal attention
-(``scaled_dot_product_attention``) is a PyTorch operation around the BitLinear
-hot path; RMSNorm, the rotary position embedding, the SwiGLU gate and the
+not stated; this is the BitNet convention).  Causal attention of rectangular
+batches with a k and v head to each q head (``scaled_dot_product_attention``) is a
+PyTorch operation around the BitLinear hot path; RMSNorm, the rotary position embedding, the SwiGLU gate and the
 token cross-entropy run on this library's decoder-support kernels (one bf16
 pass each way with fp32 arithmetic, no fp32 copies of q, k or the logits).
 
